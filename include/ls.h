@@ -261,6 +261,71 @@ int ls_generate_static(const ls_config *cfg, const ls_weights *weights, const in
                        int32_t *dev_out_tokens, ls_stats *host_stats, void *stream);
 size_t ls_static_workspace_limit(void);
 
+/* ---- Training the shared head ------------------------------------------------------------------
+ * Every exit answers with g(x_l) = W . RMSNorm(x_l), so one norm gain and one LM head W learn from the early-exit loss of
+ * Section 4.1, a sum over layers of e(l) * cross entropy of g(x_l).  These calls are the operators of that: loss, gradients and
+ * update.  They need no context, work on DEVICE memory of any sequence, only ENQUEUE on `stream` and may be recorded into a
+ * graph.  The device of the pointers must be current.  Rows (x, y, h, dx, dy, dh) are d elements each, `stride` elements apart (at least d);
+ * d is a multiple of 16 up to 65536; pointers and strides are multiples of 16 bytes; outputs may not overlap inputs or each other.
+ * A workspace is DEVICE memory, 256-byte aligned, whose contents need not survive a call; two calls that can overlap in time,
+ * and graphs that can, need one each.  LS_E_ARG: a null or misaligned pointer, an unknown dtype; LS_E_RANGE: a count or stride
+ * outside its range; LS_E_CAPACITY: workspace too small.  Results depend on the arguments' values alone, not on the call. */
+
+/* y = x * r * gain with r = 1 / sqrt(mean(x^2) + eps), rounded once.  x has x_dtype (a context's captured states are LS_F32), gain
+ * and y have `dtype`.  1 <= n <= 2^24 rows. */
+int ls_rms_norm(const void *dev_x, int32_t x_dtype, int64_t x_stride, const void *dev_gain, int32_t dtype, int32_t n,
+                int32_t d, float eps, void *dev_y, int64_t y_stride, void *stream);
+
+/* Gradients of ls_rms_norm for dy (`dtype`): dx (x_dtype; NULL: not wanted) = r (gain dy) - x r^3 mean(gain dy x) and dgain
+ * (`dtype`, [d]; NULL: not wanted, no workspace then) = sum over rows of dy x r.  Sums are fp32 in a fixed order. */
+size_t ls_rms_norm_grad_workspace(int32_t n, int32_t d);
+int ls_rms_norm_grad(const void *dev_x, int32_t x_dtype, int64_t x_stride, const void *dev_gain, int32_t dtype,
+                     const void *dev_dy, int64_t dy_stride, int32_t n, int32_t d, float eps, void *dev_dx, int64_t dx_stride,
+                     void *dev_dgain, void *dev_workspace, size_t workspace_bytes, void *stream);
+
+/* Softmax cross entropy of n rows through an LM head [vocab][d] (any vocab from 1 to 2^21), without keeping the logits:
+ * lse[i] = log sum_v exp(h_i . W_v), loss[i] = lse[i] - h_i . W_target[i], both float[n] (dev_lse may be NULL).  dev_targets: DEVICE
+ * int32[n]; a negative target skips the row (loss 0), one of vocab or more makes its loss NaN.  1 <= n <= 2^22.
+ * Products and sums are fp32 (fp32 operands: to 24 bits). */
+int ls_head_loss(const void *dev_h, int64_t h_stride, const void *dev_lm_head, int32_t dtype, const int32_t *dev_targets,
+                 int32_t n, int32_t d, int32_t vocab, float *dev_loss, float *dev_lse, void *dev_workspace,
+                 size_t workspace_bytes, void *stream);
+/* The same loss with the gradients of sum_i weight[i] * loss[i] (DEVICE float[n]; rows of several exits are stacked, with each
+ * exit's scale in its rows' weights): p = weight * (softmax - [target]), dh = p W, dW = p^T h, both in `dtype`, both overwritten; a
+ * skipped row adds nothing and its dh is 0; a target of vocab or more makes its dh and all of dW NaN.  For LS_BF16 p is
+ * rounded to 16 bits once, ahead of the two products; their sums are fp32 and are rounded once. */
+int ls_head_loss_grad(const void *dev_h, int64_t h_stride, const void *dev_lm_head, int32_t dtype, const int32_t *dev_targets,
+                      const float *dev_weight, int32_t n, int32_t d, int32_t vocab, float *dev_loss, float *dev_lse,
+                      void *dev_dh, int64_t dh_stride, void *dev_dw, void *dev_workspace, size_t workspace_bytes, void *stream);
+/* Workspace of the two calls above (with_grad 0 or 1); 0 if the sizes or the dtype are not supported. */
+size_t ls_head_loss_workspace(int32_t n, int32_t d, int32_t vocab, int32_t dtype, int32_t with_grad);
+
+/* One AdamW step over n_tensors tensors in few launches: with x = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) x;  v = beta2 v + (1 - beta2) x^2;
+ *   param = param (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * master, if not NULL, is an fp32 copy of the parameter: it is stepped, and param receives its rounding.
+ * state_bits 32: m and v are float[n].  state_bits 8: m and v are OCP e4m3 codes (bytes) of m / m_scale and sqrt(v) / v_scale, with
+ * one float scale for every 256 elements (the last block may be shorter), the largest value over 448; the step uses the
+ * unrounded values, and a root above zero is never stored as zero.  A gradient that is not finite reaches its own element of 32-bit
+ * states, and its whole block of 8-bit ones.  A recorded call repeats with the `step` and `lr` it was recorded with.
+ * The tensors of one call may not overlap.  A context reads its weight tensors anew in every call: stepping them (on the same
+ * stream, or with the streams ordered) changes what the next ls_prefill, ls_generate* or ls_score computes. */
+typedef struct {
+  void *param;                     /* DEVICE, [n], param_dtype                                   */
+  const void *grad;                /* DEVICE, [n], grad_dtype                                    */
+  float *master;                   /* DEVICE float[n] or NULL                                    */
+  void *m, *v;                     /* DEVICE, float[n] or uint8[n]                               */
+  float *m_scale, *v_scale;        /* DEVICE float[(n + 255) / 256] (8 bits), ignored otherwise   */
+  int64_t n;                       /* elements; 0: skipped                                       */
+  int32_t param_dtype, grad_dtype; /* LS_F32 or LS_BF16                                          */
+} ls_adam_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps > 0, lr and weight_decay finite and >= 0 */
+  int32_t step;                                           /* of this call, from 1               */
+  int32_t state_bits;                                     /* 32 or 8                            */
+} ls_adam_config;
+int ls_adamw(const ls_adam_tensor *host_tensors, int32_t n_tensors, const ls_adam_config *config, void *stream);
+
 const char *ls_strerror(int code);
 
 /* Frees the host object only; the workspace and the weights stay with the caller. */

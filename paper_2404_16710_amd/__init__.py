@@ -6,4 +6,5 @@ arguments: torch provides device memory and streams, nothing else.
 """
 from .binding import (  # noqa: F401
     LsError, LsModel, Stats, DeviceWeights, generate_static, lib, lib_path, config_struct, LS_F32, LS_BF16,
+    rms_norm, rms_norm_grad, head_loss, head_loss_grad, AdamW,
 )

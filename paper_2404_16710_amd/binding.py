@@ -21,6 +21,8 @@ EXPORTS = (
     "ls_generate_no_reuse", "ls_generate_dynamic", "ls_generate_early_exit", "ls_score", "ls_probe_layers", "ls_get_state", "ls_peek_round", "ls_debug_capture",
     "ls_debug_timeline", "ls_debug_copy", "ls_debug_read", "ls_set_launch", "ls_set_prompt_tiles", "ls_debug_spin_limit", "ls_debug_kv_policy", "ls_debug_prompt_plan", "ls_strerror", "ls_destroy",
     "ls_generate_static", "ls_static_workspace_limit",
+    "ls_rms_norm", "ls_rms_norm_grad", "ls_rms_norm_grad_workspace", "ls_head_loss", "ls_head_loss_grad", "ls_head_loss_workspace",
+    "ls_adamw",
 )
 
 
@@ -49,6 +51,17 @@ class ls_weights(C.Structure):
 class ls_stats(C.Structure):
     _fields_ = [("rounds", C.c_int64), ("drafted", C.c_int64), ("accepted", C.c_int64),
                 ("generated", C.c_int64), ("ms_prefill", C.c_float), ("ms_decode", C.c_float)]
+
+
+class ls_adam_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32)]
+
+
+class ls_adam_config(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + \
+               [("step", C.c_int32), ("state_bits", C.c_int32)]
 
 
 @dataclass
@@ -131,6 +144,21 @@ def lib() -> C.CDLL:
                                      C.POINTER(ls_stats), vp]
     L.ls_static_workspace_limit.restype = C.c_size_t
     L.ls_static_workspace_limit.argtypes = []
+    i64, f32, sz = C.c_int64, C.c_float, C.c_size_t
+    L.ls_rms_norm.restype = C.c_int
+    L.ls_rms_norm.argtypes = [vp, i32, i64, vp, i32, i32, i32, f32, vp, i64, vp]
+    L.ls_rms_norm_grad_workspace.restype = sz
+    L.ls_rms_norm_grad_workspace.argtypes = [i32, i32]
+    L.ls_rms_norm_grad.restype = C.c_int
+    L.ls_rms_norm_grad.argtypes = [vp, i32, i64, vp, i32, vp, i64, i32, i32, f32, vp, i64, vp, vp, sz, vp]
+    L.ls_head_loss_workspace.restype = sz
+    L.ls_head_loss_workspace.argtypes = [i32, i32, i32, i32, i32]
+    L.ls_head_loss.restype = C.c_int
+    L.ls_head_loss.argtypes = [vp, i64, vp, i32, vp, i32, i32, i32, vp, vp, vp, sz, vp]
+    L.ls_head_loss_grad.restype = C.c_int
+    L.ls_head_loss_grad.argtypes = [vp, i64, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, i64, vp, vp, sz, vp]
+    L.ls_adamw.restype = C.c_int
+    L.ls_adamw.argtypes = [C.POINTER(ls_adam_tensor), i32, C.POINTER(ls_adam_config), vp]
     L.ls_strerror.restype = C.c_char_p
     L.ls_strerror.argtypes = [C.c_int]
     L.ls_destroy.restype = None
@@ -407,3 +435,168 @@ class LsModel:
             _check(self.lib.ls_debug_capture(self.ctx, None), "ls_debug_capture")
             self._capture = None
         return self._capture
+
+
+# -- the operators that the shared head is trained with (include/ls.h): tensors in, tensors out, on the tensors' device and its
+#    current stream.  What the C interface cannot see (types, devices, shapes, strides of tensors) is checked here.
+def _dtype_of(t, what: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return LS_BF16
+    if t.dtype == torch.float32:
+        return LS_F32
+    raise ValueError(f"{what}: {t.dtype} is neither float32 nor bfloat16")
+
+
+def _rows(t, what: str, device, width: Optional[int] = None) -> int:
+    """The row stride of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
+    if t.device != device or device.type != "cuda":
+        raise ValueError(f"{what}: on {t.device}, wanted on the GPU of the first tensor ({device})")
+    if width is not None and t.shape[1] != width:
+        raise ValueError(f"{what}: rows of {t.shape[1]} elements, wanted {width}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _flat(t, what: str, device, n: int, dtype) -> int:
+    if tuple(t.shape) != (n,) or t.dtype != dtype or t.device != device or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: a contiguous {dtype} vector of {n} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _call(device, name: str, *args) -> None:
+    import torch
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            code = getattr(lib(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        code = getattr(lib(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
+    if code != 0:
+        raise LsError(code, name)
+
+
+def _result(out, what: str, like_shape, dtype, device):
+    import torch
+    if out is None:
+        return torch.empty(like_shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(like_shape) or out.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} {tuple(like_shape)} is wanted, got {out.dtype} {tuple(out.shape)}")
+    return out
+
+
+def rms_norm(x, gain, eps: float, out=None):
+    """ls_rms_norm: x [n, d] (float32 or bfloat16, rows may be strided), gain [d]; y [n, d] in the gain's type."""
+    dev, n, d = x.device, x.shape[0], x.shape[-1]
+    xs = _rows(x, "x", dev)
+    gp = _flat(gain, "gain", dev, d, gain.dtype)
+    y = _result(out, "out", (n, d), gain.dtype, dev)
+    _call(dev, "ls_rms_norm", x.data_ptr(), _dtype_of(x, "x"), xs, gp, _dtype_of(gain, "gain"), n, d, eps, y.data_ptr(),
+          _rows(y, "out", dev))
+    return y
+
+
+def rms_norm_grad(x, gain, dy, eps: float, need_dx: bool = True):
+    """ls_rms_norm_grad: (dx in x's type or None, dgain in the gain's type) for dy [n, d] in the gain's type."""
+    import torch
+    dev, n, d = x.device, x.shape[0], x.shape[-1]
+    xs = _rows(x, "x", dev)
+    gp = _flat(gain, "gain", dev, d, gain.dtype)
+    ys = _rows(dy, "dy", dev, d)
+    if dy.shape[0] != n or dy.dtype != gain.dtype:
+        raise ValueError(f"dy: {n} rows of {gain.dtype} are wanted, got {dy.dtype} {tuple(dy.shape)}")
+    dx = torch.empty((n, d), dtype=x.dtype, device=dev) if need_dx else None
+    dgain = torch.empty(d, dtype=gain.dtype, device=dev)
+    nbytes = lib().ls_rms_norm_grad_workspace(n, d)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, "ls_rms_norm_grad", x.data_ptr(), _dtype_of(x, "x"), xs, gp, _dtype_of(gain, "gain"), dy.data_ptr(), ys, n, d, eps,
+          dx.data_ptr() if need_dx else None, d, dgain.data_ptr(), ws.data_ptr(), nbytes)
+    return dx, dgain
+
+
+def _head(h, lm_head, targets):
+    import torch
+    dev, n, d, vocab = h.device, h.shape[0], h.shape[-1], lm_head.shape[0]
+    hs = _rows(h, "h", dev)
+    if _rows(lm_head, "lm_head", dev, d) != d or lm_head.dtype != h.dtype:
+        raise ValueError(f"lm_head: contiguous rows of {h.dtype} are wanted, got {lm_head.dtype}, strides {lm_head.stride()}")
+    return dev, n, d, vocab, hs, _dtype_of(h, "h"), _flat(targets, "targets", dev, n, torch.int32)
+
+
+def head_loss(h, lm_head, targets):
+    """ls_head_loss: (loss, lse), float32 [n] each, of h [n, d] through lm_head [vocab, d]; targets int32 [n], negative: skipped."""
+    import torch
+    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets)
+    loss = torch.empty(n, dtype=torch.float32, device=dev)
+    lse = torch.empty(n, dtype=torch.float32, device=dev)
+    nbytes = lib().ls_head_loss_workspace(n, d, vocab, dt, 0)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, "ls_head_loss", h.data_ptr(), hs, lm_head.data_ptr(), dt, tp, n, d, vocab, loss.data_ptr(), lse.data_ptr(),
+          ws.data_ptr(), nbytes)
+    return loss, lse
+
+
+def head_loss_grad(h, lm_head, targets, weight, d_lm_head=None):
+    """ls_head_loss_grad: (loss [n], dh [n, d], d_lm_head [vocab, d]) of sum(weight * loss); weight float32 [n].  d_lm_head: a tensor to
+    overwrite (a new one otherwise)."""
+    import torch
+    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets)
+    wp = _flat(weight, "weight", dev, n, torch.float32)
+    loss = torch.empty(n, dtype=torch.float32, device=dev)
+    dh = torch.empty((n, d), dtype=h.dtype, device=dev)
+    dw = _result(d_lm_head, "d_lm_head", (vocab, d), lm_head.dtype, dev)
+    if _rows(dw, "d_lm_head", dev, d) != d:
+        raise ValueError("d_lm_head: contiguous rows are wanted")
+    nbytes = lib().ls_head_loss_workspace(n, d, vocab, dt, 1)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call(dev, "ls_head_loss_grad", h.data_ptr(), hs, lm_head.data_ptr(), dt, tp, wp, n, d, vocab, loss.data_ptr(), None,
+          dh.data_ptr(), d, dw.data_ptr(), ws.data_ptr(), nbytes)
+    return loss, dh, dw
+
+
+class AdamW:
+    """ls_adamw over a list of tensors: parameters (updated in place), their gradients (read at every step) and the states, which
+    this object holds.  params, grads: contiguous float32 or bfloat16 tensors; masters: float32 copies of all parameters, stepped in their
+    place, or None.  bits: 32 (states {"m", "v"}, float32) or 8 ({"m", "r"}: torch.float8_e4m3fn of the first moment and of the root of
+    the second, {"m_scale", "r_scale"}: float32, one for 256 elements).  states: those of an earlier run, or None for zeros."""
+
+    def __init__(self, params, grads, masters=None, bits: int = 32, states=None, step: int = 0, lr: float = 1e-4,
+                 betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.0):
+        import torch
+        if bits not in (8, 32):
+            raise ValueError(f"bits: 8 or 32, got {bits}")
+        if not len(params) == len(grads) == len(masters if masters is not None else params) == len(states if states is not None else params):
+            raise ValueError("params, grads, masters and states: one of each for every tensor")
+        self.params, self.grads, self.masters, self.bits = list(params), list(grads), None if masters is None else list(masters), bits
+        self.steps, self.lr, self.betas, self.eps, self.weight_decay = int(step), lr, betas, eps, weight_decay
+        self.states = []
+        self._table = (ls_adam_tensor * max(1, len(self.params)))()
+        self.device = self.params[0].device if self.params else torch.device("cuda", torch.cuda.current_device())
+        e4m3 = torch.float8_e4m3fn
+        for i, p in enumerate(self.params):
+            n = p.numel()
+            st = states[i] if states is not None else (
+                {"m": torch.zeros(n, device=p.device), "v": torch.zeros(n, device=p.device)} if bits == 32 else
+                {k: torch.zeros(n if k in ("m", "r") else -(-n // 256), dtype=e4m3 if k in ("m", "r") else torch.float32, device=p.device)
+                 for k in ("m", "m_scale", "r", "r_scale")})
+            want = {"m": (n, torch.float32), "v": (n, torch.float32)} if bits == 32 else \
+                {"m": (n, e4m3), "r": (n, e4m3), "m_scale": (-(-n // 256), torch.float32), "r_scale": (-(-n // 256), torch.float32)}
+            named = [("param", p, n, p.dtype), ("grad", self.grads[i], n, self.grads[i].dtype)]
+            named += [("master", self.masters[i], n, torch.float32)] if masters is not None else []
+            named += [(k, st[k], *w) for k, w in want.items()]
+            for what, t, numel, dtype in named:
+                if t.numel() != numel or t.dtype != dtype or t.device != self.device or not t.is_contiguous() or t.device.type != "cuda":
+                    raise ValueError(f"tensor {i}, {what}: contiguous {dtype} of {numel} elements on {self.device} is wanted, "
+                                     f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+            self.states.append(st)
+            v, scales = ("v", (None, None)) if bits == 32 else ("r", (st["m_scale"].data_ptr(), st["r_scale"].data_ptr()))
+            self._table[i] = ls_adam_tensor(p.data_ptr(), self.grads[i].data_ptr(), self.masters[i].data_ptr() if masters is not None else None,
+                                            st["m"].data_ptr(), st[v].data_ptr(), *scales, n, _dtype_of(p, "param"),
+                                            _dtype_of(self.grads[i], "grad"))
+
+    def step(self, step: Optional[int] = None, grad_scale: float = 1.0) -> None:
+        """One step; `step` is its number (from 1), by default one more than the last."""
+        number = self.steps + 1 if step is None else int(step)
+        c = ls_adam_config(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, grad_scale, number, self.bits)
+        _call(self.device, "ls_adamw", self._table, len(self.params), C.byref(c))
+        self.steps = number

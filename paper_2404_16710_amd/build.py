@@ -16,7 +16,7 @@ OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libls.so")
 SOURCES = [
     "ls_kernels_bf16_hd128.hip", "ls_kernels_bf16_hd64.hip", "ls_kernels_f32_hd128.hip", "ls_kernels_f32_hd64.hip",
-    "ls_launch.hip", "ls_prefill.hip", "ls_api.cpp",
+    "ls_launch.hip", "ls_prefill.hip", "ls_train.hip", "ls_api.cpp", "ls_train_api.cpp",
 ]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -42,7 +42,7 @@ def _run(cmd, verbose):
         raise RuntimeError("hipcc failed:\n" + out)
 
 
-def build(verbose: bool = True, jobs: int = 7) -> str:
+def build(verbose: bool = True, jobs: int = 8) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
     objs = [os.path.join(OBJDIR, os.path.splitext(s)[0] + ".o") for s in SOURCES]
     cmds = [[HIPCC] + FLAGS + ["-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]

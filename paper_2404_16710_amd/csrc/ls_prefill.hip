@@ -16,6 +16,7 @@
 
 #include "ls_internal.h"
 #include "ls_lanes.h"
+#include "ls_tiles.h"
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

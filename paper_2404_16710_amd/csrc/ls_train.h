@@ -1,0 +1,39 @@
+// Launchers of the operators that the shared head is trained with (ls_train.hip), called by the C ABI after its checks.
+// All only enqueue on `stream` and return 0, or 1 when the runtime refused a launch.
+#ifndef LS_TRAIN_H_
+#define LS_TRAIN_H_
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/ls.h"
+
+struct LsNormArgs {
+  const void *x, *gain, *dy;
+  void *y, *dx, *dgain;
+  int64_t x_stride, y_stride, dy_stride, dx_stride;
+  int32_t x_bf16, bf16, n, d;
+  float eps;
+  float* partial;                 // [ls_norm_partials][d]
+};
+int ls_launch_norm(const LsNormArgs& a, hipStream_t stream);
+int ls_launch_norm_grad(const LsNormArgs& a, hipStream_t stream);
+int ls_norm_partials(int32_t n, int32_t d);
+
+struct LsHeadArgs {
+  const void *h, *lm_head;
+  const int32_t* targets;
+  const float* weight;            // null: no gradients
+  void *dh, *dw;
+  float *loss, *lse;              // (lse may be null)
+  int64_t h_stride, dh_stride;
+  int32_t bf16, n, d, vocab;
+  char* ws;
+};
+size_t ls_head_workspace(int32_t n, int32_t d, int32_t vocab, int32_t bf16, bool grad);
+int ls_launch_head(const LsHeadArgs& a, hipStream_t stream);
+
+int ls_launch_adamw(const ls_adam_tensor* t, int n_tensors, const ls_adam_config* c, hipStream_t stream);
+
+#endif

@@ -1,0 +1,81 @@
+// Operators that the shared head g (final RMSNorm + LM head) is trained with, for gfx950:
+//   * RMSNorm of rows and its gradients            y = x r g, r = 1 / sqrt(mean x^2 + eps)
+//   * softmax cross entropy through the LM head    loss = log sum exp(h W^T) - (h W^T)[target], with gradients
+//   * AdamW over many tensors, states in 32 bits or as e4m3 with a scale for 256 elements
+// Rows are independent and every sum has a fixed order: results do not change from call to call.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ls_lanes.h"
+#include "ls_tiles.h"
+#include "ls_train.h"
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t bf16_t;
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float tr_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float tr_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+// Two fp32 values as bf16, rounded to nearest even.
+__device__ __forceinline__ uint32_t tr_pack2(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// 8 consecutive elements (16-byte aligned), from and to fp32.
+struct F8 { float v[8]; };
+__device__ __forceinline__ F8 load8(const float* p) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+  return F8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+__device__ __forceinline__ F8 load8(const bf16_t* p) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p);
+  return F8{{tr_lo(a.x), tr_hi(a.x), tr_lo(a.y), tr_hi(a.y), tr_lo(a.z), tr_hi(a.z), tr_lo(a.w), tr_hi(a.w)}};
+}
+__device__ __forceinline__ void store8(float* p, const F8& f) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{f.v[0], f.v[1], f.v[2], f.v[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{f.v[4], f.v[5], f.v[6], f.v[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, const F8& f) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(tr_pack2(f.v[0], f.v[1]), tr_pack2(f.v[2], f.v[3]), tr_pack2(f.v[4], f.v[5]), tr_pack2(f.v[6], f.v[7]));
+}
+
+// Sum over the TPR threads (64 or 256) that share a row; `red`: 4 floats of LDS, free when this is called again.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if constexpr (TPR == 64) return v;
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[wave] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+#include "ls_head_mm.inc"
+#include "ls_norm.inc"
+#include "ls_head_loss.inc"
+#include "ls_adamw.inc"
+
+}  // namespace
+
+int ls_norm_partials(int32_t n, int32_t d) { return norm_partials(n, d); }
+int ls_launch_norm(const LsNormArgs& a, hipStream_t s) {
+  return a.x_bf16 ? (a.bf16 ? norm_launch<bf16_t, bf16_t>(a, s) : norm_launch<bf16_t, float>(a, s))
+                  : (a.bf16 ? norm_launch<float, bf16_t>(a, s) : norm_launch<float, float>(a, s));
+}
+int ls_launch_norm_grad(const LsNormArgs& a, hipStream_t s) {
+  return a.x_bf16 ? (a.bf16 ? norm_grad_launch<bf16_t, bf16_t>(a, s) : norm_grad_launch<bf16_t, float>(a, s))
+                  : (a.bf16 ? norm_grad_launch<float, bf16_t>(a, s) : norm_grad_launch<float, float>(a, s));
+}
+size_t ls_head_workspace(int32_t n, int32_t d, int32_t vocab, int32_t bf16, bool grad) { return head_plan(n, d, vocab, bf16 != 0, grad).total; }
+int ls_launch_head(const LsHeadArgs& a, hipStream_t s) { return a.bf16 ? head_launch<bf16_t>(a, s) : head_launch<float>(a, s); }
+int ls_launch_adamw(const ls_adam_tensor* t, int n_tensors, const ls_adam_config* c, hipStream_t s) { return adamw_launch(t, n_tensors, c, s); }

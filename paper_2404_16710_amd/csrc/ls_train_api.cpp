@@ -1,0 +1,114 @@
+// C ABI of the operators that the shared head is trained with (include/ls.h): checks of arguments, then launches.
+#include <cmath>
+#include <cstdint>
+
+#include "ls_train.h"
+
+namespace {
+
+constexpr int32_t kMaxRows = 1 << 22, kMaxNormRows = 1 << 24, kMaxWidth = 65536, kMaxVocab = 1 << 21;
+
+bool dtype_ok(int32_t t) { return t == LS_F32 || t == LS_BF16; }
+int64_t elem(int32_t t) { return t == LS_BF16 ? 2 : 4; }
+bool off16(const void* p) { return p == nullptr || (uintptr_t)p % 16 != 0; }
+bool off4(const void* p) { return p == nullptr || (uintptr_t)p % 4 != 0; }
+bool width_ok(int32_t d) { return d >= 16 && d <= kMaxWidth && d % 16 == 0; }
+bool stride_ok(int64_t stride, int32_t d, int32_t dtype) { return stride >= d && stride <= ((int64_t)1 << 20) && stride * elem(dtype) % 16 == 0; }
+bool head_sizes_ok(int32_t n, int32_t d, int32_t vocab) { return n >= 1 && n <= kMaxRows && width_ok(d) && vocab >= 1 && vocab <= kMaxVocab; }
+
+int workspace_ok(const void* ws, size_t have, size_t need) {
+  if (ws == nullptr || (uintptr_t)ws % 256) return LS_E_ARG;
+  return have < need ? LS_E_CAPACITY : LS_OK;
+}
+
+int head_call(const LsHeadArgs& a, int32_t dtype, size_t have, bool grad, void* stream) {
+  if (!dtype_ok(dtype) || off16(a.h) || off16(a.lm_head) || off4(a.targets) || off4(a.loss) || (uintptr_t)a.lse % 4) return LS_E_ARG;
+  if (grad && (off4(a.weight) || off16(a.dh) || off16(a.dw))) return LS_E_ARG;
+  if (!head_sizes_ok(a.n, a.d, a.vocab) || !stride_ok(a.h_stride, a.d, dtype)) return LS_E_RANGE;
+  if (grad && !stride_ok(a.dh_stride, a.d, dtype)) return LS_E_RANGE;
+  const int rc = workspace_ok(a.ws, have, ls_head_workspace(a.n, a.d, a.vocab, dtype == LS_BF16, grad));
+  if (rc != LS_OK) return rc;
+  return ls_launch_head(a, static_cast<hipStream_t>(stream)) == 0 ? LS_OK : LS_E_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ls_rms_norm(const void* x, int32_t x_dtype, int64_t x_stride, const void* gain, int32_t dtype, int32_t n, int32_t d, float eps,
+                void* y, int64_t y_stride, void* stream) {
+  if (!dtype_ok(x_dtype) || !dtype_ok(dtype) || off16(x) || off16(gain) || off16(y)) return LS_E_ARG;
+  if (n < 1 || n > kMaxNormRows || !width_ok(d) || !(eps > 0.f) || !stride_ok(x_stride, d, x_dtype) || !stride_ok(y_stride, d, dtype))
+    return LS_E_RANGE;
+  LsNormArgs a{};
+  a.x = x; a.gain = gain; a.y = y; a.x_stride = x_stride; a.y_stride = y_stride;
+  a.x_bf16 = x_dtype == LS_BF16; a.bf16 = dtype == LS_BF16; a.n = n; a.d = d; a.eps = eps;
+  return ls_launch_norm(a, static_cast<hipStream_t>(stream)) == 0 ? LS_OK : LS_E_HIP;
+}
+
+size_t ls_rms_norm_grad_workspace(int32_t n, int32_t d) {
+  if (n < 1 || n > kMaxNormRows || !width_ok(d)) return 0;
+  return sizeof(float) * (size_t)ls_norm_partials(n, d) * d;
+}
+
+int ls_rms_norm_grad(const void* x, int32_t x_dtype, int64_t x_stride, const void* gain, int32_t dtype, const void* dy, int64_t dy_stride,
+                     int32_t n, int32_t d, float eps, void* dx, int64_t dx_stride, void* dgain, void* ws, size_t bytes, void* stream) {
+  if (!dtype_ok(x_dtype) || !dtype_ok(dtype) || off16(x) || off16(gain) || off16(dy)) return LS_E_ARG;
+  if ((dx == nullptr && dgain == nullptr) || (uintptr_t)dx % 16 || (uintptr_t)dgain % 16) return LS_E_ARG;
+  if (n < 1 || n > kMaxNormRows || !width_ok(d) || !(eps > 0.f) || !stride_ok(x_stride, d, x_dtype) || !stride_ok(dy_stride, d, dtype))
+    return LS_E_RANGE;
+  if (dx != nullptr && !stride_ok(dx_stride, d, x_dtype)) return LS_E_RANGE;
+  if (dgain != nullptr) {
+    const int rc = workspace_ok(ws, bytes, ls_rms_norm_grad_workspace(n, d));
+    if (rc != LS_OK) return rc;
+  }
+  LsNormArgs a{};
+  a.x = x; a.gain = gain; a.dy = dy; a.dx = dx; a.dgain = dgain;
+  a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
+  a.x_bf16 = x_dtype == LS_BF16; a.bf16 = dtype == LS_BF16; a.n = n; a.d = d; a.eps = eps;
+  a.partial = static_cast<float*>(ws);
+  return ls_launch_norm_grad(a, static_cast<hipStream_t>(stream)) == 0 ? LS_OK : LS_E_HIP;
+}
+
+size_t ls_head_loss_workspace(int32_t n, int32_t d, int32_t vocab, int32_t dtype, int32_t with_grad) {
+  if (!dtype_ok(dtype) || !head_sizes_ok(n, d, vocab) || with_grad < 0 || with_grad > 1) return 0;
+  return ls_head_workspace(n, d, vocab, dtype == LS_BF16, with_grad != 0);
+}
+
+int ls_head_loss(const void* h, int64_t h_stride, const void* lm_head, int32_t dtype, const int32_t* targets, int32_t n, int32_t d,
+                 int32_t vocab, float* loss, float* lse, void* ws, size_t bytes, void* stream) {
+  LsHeadArgs a{};
+  a.h = h; a.lm_head = lm_head; a.targets = targets; a.loss = loss; a.lse = lse;
+  a.h_stride = h_stride; a.bf16 = dtype == LS_BF16; a.n = n; a.d = d; a.vocab = vocab; a.ws = static_cast<char*>(ws);
+  return head_call(a, dtype, bytes, false, stream);
+}
+
+int ls_head_loss_grad(const void* h, int64_t h_stride, const void* lm_head, int32_t dtype, const int32_t* targets, const float* weight,
+                      int32_t n, int32_t d, int32_t vocab, float* loss, float* lse, void* dh, int64_t dh_stride, void* dw, void* ws,
+                      size_t bytes, void* stream) {
+  LsHeadArgs a{};
+  a.h = h; a.lm_head = lm_head; a.targets = targets; a.weight = weight; a.loss = loss; a.lse = lse; a.dh = dh; a.dw = dw;
+  a.h_stride = h_stride; a.dh_stride = dh_stride; a.bf16 = dtype == LS_BF16; a.n = n; a.d = d; a.vocab = vocab;
+  a.ws = static_cast<char*>(ws);
+  return head_call(a, dtype, bytes, true, stream);
+}
+
+int ls_adamw(const ls_adam_tensor* t, int32_t n_tensors, const ls_adam_config* c, void* stream) {
+  if (!c || (n_tensors > 0 && !t)) return LS_E_ARG;
+  if (n_tensors < 0 || c->step < 1) return LS_E_RANGE;
+  if (c->state_bits != 32 && c->state_bits != 8) return LS_E_ARG;
+  auto share = [](double b) { return b >= 0.0 && b < 1.0; };
+  if (!share(c->beta1) || !share(c->beta2) || !(c->eps > 0.0) || !(c->lr >= 0.0) || !(c->weight_decay >= 0.0) || !std::isfinite(c->lr) ||
+      !std::isfinite(c->eps) || !std::isfinite(c->weight_decay) || !std::isfinite(c->grad_scale))
+    return LS_E_RANGE;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 42)) return LS_E_RANGE;
+    if (t[i].n == 0) continue;
+    if (!dtype_ok(t[i].param_dtype) || !dtype_ok(t[i].grad_dtype)) return LS_E_ARG;
+    if (off16(t[i].param) || off16(t[i].grad) || off16(t[i].m) || off16(t[i].v) || (uintptr_t)t[i].master % 16) return LS_E_ARG;
+    if (c->state_bits == 8 && (off4(t[i].m_scale) || off4(t[i].v_scale))) return LS_E_ARG;
+  }
+  return ls_launch_adamw(t, n_tensors, c, static_cast<hipStream_t>(stream)) == 0 ? LS_OK : LS_E_HIP;
+}
+
+}  // extern "C"

@@ -300,6 +300,19 @@ int ls_head_loss_grad(const void *dev_h, int64_t h_stride, const void *dev_lm_he
 /* Workspace of the two calls above (with_grad 0 or 1); 0 if the sizes or the dtype are not supported. */
 size_t ls_head_loss_workspace(int32_t n, int32_t d, int32_t vocab, int32_t dtype, int32_t with_grad);
 
+/* The early-exit loss of a text (Section 4.1): tokens (DEVICE int32[n]) run through the layers as one causal sequence from position
+ * 0, g is applied to the output of every layer l with host_scale[l] != 0 (HOST float[n_layers]; l = 0 is the first layer's output), and
+ * dev_loss, DEVICE float[exits][n] in layer order, receives the cross entropy of every row against dev_targets (DEVICE int32[n]; usually
+ * the next token; negative: the row is skipped), unscaled.  dev_d_lm_head ([vocab][d_model]) and dev_d_final_norm ([d_model]),
+ * in the model's dtype, receive the gradients of sum_l host_scale[l] * sum_i loss[l][i] with respect to the shared head, or are both
+ * NULL.  d_model is at most 65536, vocab 2^21, exits * n 2^22.  dev_workspace: DEVICE, 256-byte aligned, ls_exit_loss_workspace bytes (0: the
+ * arguments are not supported); it holds the captured states of the layers (for this call ls_debug_capture's buffer is not
+ * written).  Overwrites the KV cache and invalidates the decoding state.  Synchronises. */
+int ls_exit_loss(ls_ctx *ctx, const int32_t *dev_tokens, const int32_t *dev_targets, int32_t n, const float *host_scale,
+                 float *dev_loss, void *dev_d_lm_head, void *dev_d_final_norm, void *dev_workspace, size_t workspace_bytes,
+                 void *stream);
+size_t ls_exit_loss_workspace(const ls_ctx *ctx, int32_t n, const float *host_scale, int32_t with_grad);
+
 /* One AdamW step over n_tensors tensors in few launches: with x = grad * grad_scale
  *   m = beta1 m + (1 - beta1) x;  v = beta2 v + (1 - beta2) x^2;
  *   param = param (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
@@ -310,7 +323,7 @@ size_t ls_head_loss_workspace(int32_t n, int32_t d, int32_t vocab, int32_t dtype
  * states, and its whole block of 8-bit ones.  A recorded call repeats with the `step` and `lr` it was recorded with.
  * The tensors of one call may not overlap.  A context reads its weight tensors anew in every call: stepping them (on the same
  * stream, or with the streams ordered) changes what the next ls_prefill, ls_generate* or ls_score computes. */
-typedef struct {
+typedef struct { /* of one tensor */
   void *param;                     /* DEVICE, [n], param_dtype                                   */
   const void *grad;                /* DEVICE, [n], grad_dtype                                    */
   float *master;                   /* DEVICE float[n] or NULL                                    */

@@ -22,7 +22,7 @@ EXPORTS = (
     "ls_debug_timeline", "ls_debug_copy", "ls_debug_read", "ls_set_launch", "ls_set_prompt_tiles", "ls_debug_spin_limit", "ls_debug_kv_policy", "ls_debug_prompt_plan", "ls_strerror", "ls_destroy",
     "ls_generate_static", "ls_static_workspace_limit",
     "ls_rms_norm", "ls_rms_norm_grad", "ls_rms_norm_grad_workspace", "ls_head_loss", "ls_head_loss_grad", "ls_head_loss_workspace",
-    "ls_adamw",
+    "ls_adamw", "ls_exit_loss", "ls_exit_loss_workspace",
 )
 
 
@@ -157,6 +157,10 @@ def lib() -> C.CDLL:
     L.ls_head_loss.argtypes = [vp, i64, vp, i32, vp, i32, i32, i32, vp, vp, vp, sz, vp]
     L.ls_head_loss_grad.restype = C.c_int
     L.ls_head_loss_grad.argtypes = [vp, i64, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, i64, vp, vp, sz, vp]
+    L.ls_exit_loss.restype = C.c_int
+    L.ls_exit_loss.argtypes = [vp, vp, vp, i32, f32p, vp, vp, vp, vp, sz, vp]
+    L.ls_exit_loss_workspace.restype = sz
+    L.ls_exit_loss_workspace.argtypes = [vp, i32, f32p, i32]
     L.ls_adamw.restype = C.c_int
     L.ls_adamw.argtypes = [C.POINTER(ls_adam_tensor), i32, C.POINTER(ls_adam_config), vp]
     L.ls_strerror.restype = C.c_char_p
@@ -391,6 +395,45 @@ class LsModel:
         _check(self.lib.ls_probe_layers(self.ctx, C.c_void_p(t.data_ptr()), n, C.c_void_p(am.data_ptr()),
                                         C.c_void_p(mg.data_ptr()), self._stream()), "ls_probe_layers")
         return am.cpu().numpy(), mg.cpu().numpy()
+
+    def exit_loss(self, tokens: Sequence[int], scales: dict, targets: Optional[Sequence[int]] = None, d_lm_head=None, d_final_norm=None):
+        """Early-exit loss of a text.  scales: {exit layer E (1..L): its scale}; targets: one id per token, negative to skip it, by default
+        the next token (the last is skipped).  Returns the losses [exits][n] in the order of the layers, and, with the two tensors
+        d_lm_head and d_final_norm, overwrites them with the gradients of sum_E scale * (mean loss over the targets that count)."""
+        n, L = len(tokens), self.cfg.n_layers
+        if targets is None:
+            targets = [*tokens[1:], -1]
+        if len(targets) != n or not scales or any(not 1 <= e <= L for e in scales) or (d_lm_head is None) != (d_final_norm is None):
+            raise ValueError("exit_loss: a target for every token, exits from 1 to the number of layers, both gradients or neither")
+        by_name = self._dev_weights.by_name
+        for got, name in ((d_lm_head, "lm_head"), (d_final_norm, "final_norm")):
+            w = by_name[(name, -1)]
+            if got is not None and (got.shape != w.shape or got.dtype != w.dtype or got.device != w.device or not got.is_contiguous()):
+                raise ValueError(f"exit_loss: the gradient of {name} is a contiguous {w.dtype} {tuple(w.shape)} on {w.device}")
+        counted = max(1, sum(1 for t in targets if t >= 0))
+        scale = (C.c_float * L)(*[scales.get(l + 1, 0.0) / counted for l in range(L)])
+        nbytes = self.lib.ls_exit_loss_workspace(self.ctx, n, scale, 0 if d_lm_head is None else 1)
+        t, y = self._dev_i32(tokens), self._dev_i32(targets)
+        loss = self.torch.empty((sum(1 for s in scale if s != 0), n), dtype=self.torch.float32, device=self.device)
+        ws = self.torch.empty(max(256, nbytes), dtype=self.torch.uint8, device=self.device)
+        ptr = lambda x: None if x is None else x.data_ptr()  # noqa: E731
+        _check(self.lib.ls_exit_loss(self.ctx, t.data_ptr(), y.data_ptr(), n, scale, loss.data_ptr(), ptr(d_lm_head), ptr(d_final_norm),
+                                     ws.data_ptr(), nbytes, self._stream()), "ls_exit_loss")
+        return loss.cpu().numpy()
+
+    def head_optimizer(self, bits: int = 32, **kw) -> "AdamW":
+        """AdamW over this model's shared head (LM head and final norm), with gradient tensors of its own and, for a 16-bit model,
+        fp32 copies of both.  kw: lr, betas, eps, weight_decay."""
+        ws = [self._dev_weights.by_name[(name, -1)] for name in ("lm_head", "final_norm")]
+        masters = None if ws[0].dtype == self.torch.float32 else [w.float() for w in ws]
+        return AdamW(ws, [self.torch.zeros_like(w) for w in ws], masters=masters, bits=bits, **kw)
+
+    def fit_exits(self, tokens: Sequence[int], scales: dict, optimizer: "AdamW", targets: Optional[Sequence[int]] = None):
+        """One training step of the shared head on a text: losses and gradients at the exits, then the optimizer's step (head_optimizer),
+        in place: the next call answers with the new head.  Returns the losses ahead of the step, as exit_loss."""
+        losses = self.exit_loss(tokens, scales, targets, *optimizer.grads)
+        optimizer.step()
+        return losses
 
     def get_state(self):
         pos, last, n_gen = C.c_int32(), C.c_int32(), C.c_int32()

@@ -13,6 +13,7 @@
 
 #include "../../include/ls.h"
 #include "ls_internal.h"
+#include "ls_train.h"
 
 extern "C" int ls_launch_program(const LsKParams* p, int dtype_is_bf16, int grid, hipStream_t stream);
 extern "C" int ls_kernel_setup(int dtype_is_bf16, int hd, int* max_blocks_per_cu);
@@ -495,32 +496,144 @@ int ls_generate_early_exit(ls_ctx* c, const int32_t* dev_prompt, int32_t n_promp
   return generate_impl(c, dev_prompt, n_prompt, max_new, E, 0, -1, E, dev_out, stats, stream);
 }
 
+// Enqueues the layers over a text and, in the wide pass only where dev_argmax is wanted (`states_only`: it is scratch), the head.
+static int enqueue_score(ls_ctx* c, const int32_t* dev_tokens, int32_t n, int32_t layers_used, int32_t* dev_argmax, float* dev_margin,
+                         bool probe, float* capture, bool states_only, hipStream_t s) {
+  int rc = recover(c, s);
+  if (rc != LS_OK) return rc;
+  if (wide_rows(c, n)) {
+    LsPfParams f = c->pf;
+    f.ssq_nt = c->base.ssq_nt; f.tokens = dev_tokens; f.layers_used = layers_used; f.capture = capture;
+    LsScore sc = wide_pass(c, n);
+    sc.probe = probe ? 1 : 0; sc.out_tokens = states_only ? nullptr : dev_argmax; sc.out_margin = dev_margin;
+    if (ls_score_rows(&f, c->host_layers.data(), &sc, c->lay.pf_rows, s) != 0) return LS_E_HIP;
+  } else {
+    LsKParams p = program(c, LS_PROG_SCORE);
+    p.probe = probe ? 1 : 0; p.capture = capture;
+    p.tokens = dev_tokens; p.n_tokens = n; p.layers_used = layers_used; p.out_tokens = dev_argmax; p.out_margin = dev_margin;
+    rc = launch(c, p, s);
+    if (rc != LS_OK) return rc;
+  }
+  c->prefilled = false; c->drafted = false;
+  return LS_OK;
+}
+
 static int score_impl(ls_ctx* c, const int32_t* dev_tokens, int32_t n, int32_t layers_used, int32_t* dev_argmax,
                       float* dev_margin, void* stream, bool probe) {
   if (!c || !dev_tokens || !dev_argmax) return LS_E_ARG;
   if (n < 1 || layers_used < 1 || layers_used > c->cfg.n_layers) return LS_E_RANGE;
   if (n > c->cfg.max_seq) return LS_E_CAPACITY;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  int rc = recover(c, s);
+  int rc = enqueue_score(c, dev_tokens, n, layers_used, dev_argmax, dev_margin, probe, c->capture, false, s);
   if (rc != LS_OK) return rc;
-  if (wide_rows(c, n)) {
-    LsPfParams f = c->pf;
-    f.ssq_nt = c->base.ssq_nt; f.tokens = dev_tokens; f.layers_used = layers_used; f.capture = c->capture;
-    LsScore sc = wide_pass(c, n);
-    sc.probe = probe ? 1 : 0; sc.out_tokens = dev_argmax; sc.out_margin = dev_margin;
-    if (ls_score_rows(&f, c->host_layers.data(), &sc, c->lay.pf_rows, s) != 0) return LS_E_HIP;
-  } else {
-    LsKParams p = program(c, LS_PROG_SCORE);
-    p.probe = probe ? 1 : 0;
-    p.tokens = dev_tokens; p.n_tokens = n; p.layers_used = layers_used; p.out_tokens = dev_argmax; p.out_margin = dev_margin;
-    rc = launch(c, p, s);
-    if (rc != LS_OK) return rc;
-  }
-  c->prefilled = false; c->drafted = false;
   LsState st;
   rc = read_state(c, &st, s);
   if (rc != LS_OK) return rc;
   return st.error ? LS_E_DEVICE : LS_OK;
+}
+
+// What ls_exit_loss runs and where its workspace holds what; valid = the arguments are supported.
+struct ExitPlan {
+  bool valid;
+  std::vector<int> layers;           // exits, as layer indices
+  std::vector<float> scales;
+  size_t hidden, h, dh, targets, weight, argmax, head, partial, total;
+  int rows, parts;                   // exits * n; shares of the gain's gradient per exit
+};
+
+static ExitPlan exit_plan(const ls_ctx* c, int32_t n, const float* host_scale, bool grad) {
+  ExitPlan e{};
+  const ls_config& g = c->cfg;
+  const int L = g.n_layers;
+  for (int l = 0; l < L; ++l) {
+    if (!std::isfinite(host_scale[l])) return e;
+    if (host_scale[l] != 0.f) { e.layers.push_back(l); e.scales.push_back(host_scale[l]); }
+  }
+  const int64_t rows = (int64_t)e.layers.size() * n;
+  if (n < 1 || e.layers.empty() || rows > (1 << 22)) return e;
+  const size_t head = ls_head_loss_workspace((int32_t)rows, g.d_model, g.vocab, g.dtype, grad ? 1 : 0);
+  if (head == 0) return e;
+  e.rows = (int)rows;
+  e.parts = ls_norm_partials(n, g.d_model);
+  const size_t esz = g.dtype == LS_BF16 ? 2 : 4;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+  e.hidden = take(sizeof(float) * (e.layers.back() + 1) * (size_t)g.max_seq * g.d_model);
+  e.h = take(esz * rows * g.d_model);
+  e.targets = take(sizeof(int32_t) * rows);
+  e.weight = take(sizeof(float) * rows);
+  e.argmax = take(sizeof(int32_t) * n);
+  e.head = take(head);
+  if (grad) {
+    e.dh = take(esz * rows * g.d_model);
+    e.partial = take(sizeof(float) * e.layers.size() * (size_t)e.parts * g.d_model);
+  }
+  e.total = off;
+  e.valid = true;
+  return e;
+}
+
+size_t ls_exit_loss_workspace(const ls_ctx* c, int32_t n, const float* host_scale, int32_t with_grad) {
+  if (!c || !host_scale || with_grad < 0 || with_grad > 1 || n < 1 || n > c->cfg.max_seq) return 0;
+  try {
+    const ExitPlan e = exit_plan(c, n, host_scale, with_grad != 0);
+    return e.valid ? e.total : 0;
+  } catch (...) { return 0; }          // (out of host memory)
+}
+
+static int exit_loss_impl(ls_ctx* c, const int32_t* dev_tokens, const int32_t* dev_targets, int32_t n, const float* host_scale, float* dev_loss,
+                          void* dev_dw, void* dev_dgain, void* dev_ws, size_t bytes, hipStream_t s) {
+  const bool grad = dev_dw != nullptr;
+  const ExitPlan e = exit_plan(c, n, host_scale, grad);
+  if (!e.valid) return LS_E_RANGE;
+  if (bytes < e.total) return LS_E_CAPACITY;
+  const ls_config& g = c->cfg;
+  char* const ws = static_cast<char*>(dev_ws);
+  const int32_t bf16 = g.dtype == LS_BF16;
+  const size_t dm = g.d_model, row = (bf16 ? 2 : 4) * dm;
+  float* const hidden = reinterpret_cast<float*>(ws + e.hidden);
+  int32_t* const targets = reinterpret_cast<int32_t*>(ws + e.targets);
+  float* const weight = reinterpret_cast<float*>(ws + e.weight);
+  const int exits = (int)e.layers.size();
+  int rc = enqueue_score(c, dev_tokens, n, e.layers.back() + 1, reinterpret_cast<int32_t*>(ws + e.argmax), nullptr, false, hidden, true, s);
+  if (rc != LS_OK) return rc;
+  if (ls_launch_exit_rows(dev_targets, n, exits, e.scales.data(), targets, weight, s) != 0) return LS_E_HIP;
+  auto states = [&](int i) { return hidden + (size_t)e.layers[i] * g.max_seq * dm; };
+  for (int i = 0; i < exits && rc == LS_OK; ++i)
+    rc = ls_rms_norm(states(i), LS_F32, dm, c->base.final_norm, g.dtype, n, g.d_model, g.rms_eps, ws + e.h + (size_t)i * n * row, dm, s);
+  if (rc != LS_OK) return rc;
+  if (!grad) {
+    rc = ls_head_loss(ws + e.h, dm, c->base.lm_head, g.dtype, targets, e.rows, g.d_model, g.vocab, dev_loss, nullptr, ws + e.head, bytes - e.head, s);
+  } else {
+    rc = ls_head_loss_grad(ws + e.h, dm, c->base.lm_head, g.dtype, targets, weight, e.rows, g.d_model, g.vocab, dev_loss, nullptr, ws + e.dh, dm,
+                           dev_dw, ws + e.head, bytes - e.head, s);
+    // every exit's rows leave their shares of the gain's gradient behind those of the exits before
+    for (int i = 0; i < exits && rc == LS_OK; ++i) {
+      LsNormArgs a{};
+      a.x = states(i); a.gain = c->base.final_norm; a.dy = ws + e.dh + (size_t)i * n * row;
+      a.x_stride = a.dy_stride = (int64_t)dm; a.bf16 = bf16; a.n = n; a.d = g.d_model; a.eps = g.rms_eps;
+      a.partial = reinterpret_cast<float*>(ws + e.partial) + (size_t)i * e.parts * dm;
+      if (ls_launch_norm_grad(a, s) != 0) rc = LS_E_HIP;
+    }
+    if (rc == LS_OK && ls_launch_norm_gain(reinterpret_cast<float*>(ws + e.partial), exits * e.parts, g.d_model, bf16, dev_dgain, s) != 0) rc = LS_E_HIP;
+  }
+  if (rc != LS_OK) return rc;
+  LsState st;
+  rc = read_state(c, &st, s);
+  if (rc != LS_OK) return rc;
+  return st.error ? LS_E_DEVICE : LS_OK;
+}
+
+int ls_exit_loss(ls_ctx* c, const int32_t* dev_tokens, const int32_t* dev_targets, int32_t n, const float* host_scale, float* dev_loss,
+                 void* dev_dw, void* dev_dgain, void* dev_ws, size_t bytes, void* stream) {
+  if (!c || !dev_tokens || !dev_targets || !host_scale || !dev_loss || !dev_ws || (uintptr_t)dev_ws % 256) return LS_E_ARG;
+  if ((dev_dw == nullptr) != (dev_dgain == nullptr) || ((uintptr_t)dev_dw | (uintptr_t)dev_dgain) % 16) return LS_E_ARG;
+  if (((uintptr_t)dev_targets | (uintptr_t)dev_loss) % 4) return LS_E_ARG;
+  if (n < 1) return LS_E_RANGE;
+  if (n > c->cfg.max_seq) return LS_E_CAPACITY;
+  try {
+    return exit_loss_impl(c, dev_tokens, dev_targets, n, host_scale, dev_loss, dev_dw, dev_dgain, dev_ws, bytes, static_cast<hipStream_t>(stream));
+  } catch (...) { return LS_E_ARG; }   // (out of host memory; nothing has been enqueued)
 }
 
 int ls_score(ls_ctx* c, const int32_t* dev_tokens, int32_t n, int32_t layers_used, int32_t* dev_argmax,

@@ -121,7 +121,7 @@ struct LsScore {
   int32_t attn_ctiles, x_tiles;       // LsKParams: what the order of the decode kernels' sums depends on
   float attn_scale;
   const void *final_norm, *lm_head;
-  int32_t *out_tokens;
+  int32_t *out_tokens;                // null: no head (states only, through LsPfParams::capture)
   float *out_margin;
   LsState *state;
   int32_t prompt, eos, max_new;       // a prompt's rows: ends with the state of a finished prompt pass, first token to out_first

@@ -15,11 +15,13 @@ struct LsNormArgs {
   int64_t x_stride, y_stride, dy_stride, dx_stride;
   int32_t x_bf16, bf16, n, d;
   float eps;
-  float* partial;                 // [ls_norm_partials][d]
+  float* partial;                 // [ls_norm_partials][d]: the rows' share of dgain
 };
 int ls_launch_norm(const LsNormArgs& a, hipStream_t stream);
 int ls_launch_norm_grad(const LsNormArgs& a, hipStream_t stream);
+int ls_launch_norm_gain(const float* partial, int parts, int32_t d, int32_t bf16, void* dgain, hipStream_t stream);   // dgain from the shares
 int ls_norm_partials(int32_t n, int32_t d);
+int ls_launch_exit_rows(const int32_t* targets, int32_t n, int32_t exits, const float* host_scale, int32_t* out_targets, float* out_weight, hipStream_t stream);
 
 struct LsHeadArgs {
   const void *h, *lm_head;

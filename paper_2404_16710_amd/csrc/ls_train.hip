@@ -65,6 +65,12 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 #include "ls_head_loss.inc"
 #include "ls_adamw.inc"
 
+// Targets and weights of one exit's rows.
+__global__ __launch_bounds__(256) void exit_rows_kernel(const int32_t* targets, int n, float scale, int32_t* out_targets, float* out_weight) {
+  const int i = (int)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) { out_targets[i] = targets[i]; out_weight[i] = scale; }
+}
+
 }  // namespace
 
 int ls_norm_partials(int32_t n, int32_t d) { return norm_partials(n, d); }
@@ -75,6 +81,20 @@ int ls_launch_norm(const LsNormArgs& a, hipStream_t s) {
 int ls_launch_norm_grad(const LsNormArgs& a, hipStream_t s) {
   return a.x_bf16 ? (a.bf16 ? norm_grad_launch<bf16_t, bf16_t>(a, s) : norm_grad_launch<bf16_t, float>(a, s))
                   : (a.bf16 ? norm_grad_launch<float, bf16_t>(a, s) : norm_grad_launch<float, float>(a, s));
+}
+int ls_launch_norm_gain(const float* partial, int parts, int32_t d, int32_t bf16, void* dgain, hipStream_t s) {
+  const dim3 grid((d / 4 + 15) / 16);
+  if (bf16) norm_gain_kernel<bf16_t><<<grid, dim3(256), 0, s>>>(partial, parts, d, static_cast<bf16_t*>(dgain));
+  else norm_gain_kernel<float><<<grid, dim3(256), 0, s>>>(partial, parts, d, static_cast<float*>(dgain));
+  return hipGetLastError() == hipSuccess ? 0 : 1;
+}
+int ls_launch_exit_rows(const int32_t* targets, int32_t n, int32_t exits, const float* host_scale, int32_t* out_targets, float* out_weight,
+                        hipStream_t s) {
+  for (int e = 0; e < exits; ++e) {
+    exit_rows_kernel<<<dim3((n + 255) / 256), dim3(256), 0, s>>>(targets, n, host_scale[e], out_targets + (int64_t)e * n, out_weight + (int64_t)e * n);
+    if (hipGetLastError() != hipSuccess) return 1;
+  }
+  return 0;
 }
 size_t ls_head_workspace(int32_t n, int32_t d, int32_t vocab, int32_t bf16, bool grad) { return head_plan(n, d, vocab, bf16 != 0, grad).total; }
 int ls_launch_head(const LsHeadArgs& a, hipStream_t s) { return a.bf16 ? head_launch<bf16_t>(a, s) : head_launch<float>(a, s); }

@@ -66,8 +66,11 @@ int ls_rms_norm_grad(const void* x, int32_t x_dtype, int64_t x_stride, const voi
   a.x = x; a.gain = gain; a.dy = dy; a.dx = dx; a.dgain = dgain;
   a.x_stride = x_stride; a.dy_stride = dy_stride; a.dx_stride = dx_stride;
   a.x_bf16 = x_dtype == LS_BF16; a.bf16 = dtype == LS_BF16; a.n = n; a.d = d; a.eps = eps;
-  a.partial = static_cast<float*>(ws);
-  return ls_launch_norm_grad(a, static_cast<hipStream_t>(stream)) == 0 ? LS_OK : LS_E_HIP;
+  a.partial = dgain != nullptr ? static_cast<float*>(ws) : nullptr;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (ls_launch_norm_grad(a, s) != 0) return LS_E_HIP;
+  if (dgain != nullptr && ls_launch_norm_gain(a.partial, ls_norm_partials(n, d), d, a.bf16, dgain, s) != 0) return LS_E_HIP;
+  return LS_OK;
 }
 
 size_t ls_head_loss_workspace(int32_t n, int32_t d, int32_t vocab, int32_t dtype, int32_t with_grad) {

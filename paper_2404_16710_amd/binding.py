@@ -481,75 +481,78 @@ class LsModel:
 
 
 # -- the operators that the shared head is trained with (include/ls.h): tensors in, tensors out, on the tensors' device and its
-#    current stream.  What the C interface cannot see (types, devices, shapes, strides of tensors) is checked here.
+#    current stream.  What the C interface cannot see (types, devices, shapes, strides of tensors) is checked here.  Small calls
+#    are bound by these lines and the launch (a row's norm: 7 us, 3.5 of them the C call), hence one look at each property.
+_DTYPES: dict = {}
+
+
 def _dtype_of(t, what: str) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return LS_BF16
-    if t.dtype == torch.float32:
-        return LS_F32
-    raise ValueError(f"{what}: {t.dtype} is neither float32 nor bfloat16")
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: LS_F32, torch.bfloat16: LS_BF16})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: {t.dtype} is neither float32 nor bfloat16")
+    return code
 
 
-def _rows(t, what: str, device, width: Optional[int] = None) -> int:
-    """The row stride of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
-    if t.device != device or device.type != "cuda":
-        raise ValueError(f"{what}: on {t.device}, wanted on the GPU of the first tensor ({device})")
-    if width is not None and t.shape[1] != width:
-        raise ValueError(f"{what}: rows of {t.shape[1]} elements, wanted {width}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+def _rows(t, what: str, device=None, shape=(None, None)):
+    """Rows, columns and row stride of a matrix whose rows are contiguous.  device: that of the call's first tensor."""
+    size, strides = t.shape, t.stride()
+    if len(size) != 2 or (strides[1] != 1 and size[1] > 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(size)}, strides {strides}")
+    n, d = size
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{what}: on {t.device}, wanted on the GPU{'' if device is None else f' of the first tensor ({device})'}")
+    if (shape[0] is not None and n != shape[0]) or (shape[1] is not None and d != shape[1]):
+        raise ValueError(f"{what}: shape {tuple(size)}, wanted {shape}")
+    return n, d, strides[0] if n > 1 else d
 
 
 def _flat(t, what: str, device, n: int, dtype) -> int:
-    if tuple(t.shape) != (n,) or t.dtype != dtype or t.device != device or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or t.dtype != dtype or t.device != device or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{what}: a contiguous {dtype} vector of {n} on {device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _call(device, name: str, *args) -> None:
     import torch
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(index)   # (what torch.cuda.current_stream wraps, at a twentieth of its time)
+    if index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            code = getattr(lib(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
+            code = fn(*args, stream)
     else:
-        code = getattr(lib(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
+        code = fn(*args, stream)
     if code != 0:
         raise LsError(code, name)
 
 
-def _result(out, what: str, like_shape, dtype, device):
-    import torch
-    if out is None:
-        return torch.empty(like_shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(like_shape) or out.dtype != dtype:
-        raise ValueError(f"{what}: {dtype} {tuple(like_shape)} is wanted, got {out.dtype} {tuple(out.shape)}")
-    return out
-
-
 def rms_norm(x, gain, eps: float, out=None):
     """ls_rms_norm: x [n, d] (float32 or bfloat16, rows may be strided), gain [d]; y [n, d] in the gain's type."""
-    dev, n, d = x.device, x.shape[0], x.shape[-1]
-    xs = _rows(x, "x", dev)
-    gp = _flat(gain, "gain", dev, d, gain.dtype)
-    y = _result(out, "out", (n, d), gain.dtype, dev)
-    _call(dev, "ls_rms_norm", x.data_ptr(), _dtype_of(x, "x"), xs, gp, _dtype_of(gain, "gain"), n, d, eps, y.data_ptr(),
-          _rows(y, "out", dev))
-    return y
+    dev, (n, d, xs) = x.device, _rows(x, "x")
+    dtype = gain.dtype
+    gp = _flat(gain, "gain", dev, d, dtype)
+    if out is None:
+        out, ys = gain.new_empty((n, d)), d
+    else:
+        ys = _rows(out, "out", dev, (n, d))[2]
+        if out.dtype != dtype:
+            raise ValueError(f"out: {dtype} is wanted, got {out.dtype}")
+    _call(dev, "ls_rms_norm", x.data_ptr(), _dtype_of(x, "x"), xs, gp, _dtype_of(gain, "gain"), n, d, eps, out.data_ptr(), ys)
+    return out
 
 
 def rms_norm_grad(x, gain, dy, eps: float, need_dx: bool = True):
     """ls_rms_norm_grad: (dx in x's type or None, dgain in the gain's type) for dy [n, d] in the gain's type."""
     import torch
-    dev, n, d = x.device, x.shape[0], x.shape[-1]
-    xs = _rows(x, "x", dev)
+    dev, (n, d, xs) = x.device, _rows(x, "x")
     gp = _flat(gain, "gain", dev, d, gain.dtype)
-    ys = _rows(dy, "dy", dev, d)
-    if dy.shape[0] != n or dy.dtype != gain.dtype:
-        raise ValueError(f"dy: {n} rows of {gain.dtype} are wanted, got {dy.dtype} {tuple(dy.shape)}")
-    dx = torch.empty((n, d), dtype=x.dtype, device=dev) if need_dx else None
-    dgain = torch.empty(d, dtype=gain.dtype, device=dev)
+    ys = _rows(dy, "dy", dev, (n, d))[2]
+    if dy.dtype != gain.dtype:
+        raise ValueError(f"dy: {gain.dtype} is wanted, got {dy.dtype}")
+    dx = x.new_empty((n, d)) if need_dx else None
+    dgain = gain.new_empty(d)
     nbytes = lib().ls_rms_norm_grad_workspace(n, d)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _call(dev, "ls_rms_norm_grad", x.data_ptr(), _dtype_of(x, "x"), xs, gp, _dtype_of(gain, "gain"), dy.data_ptr(), ys, n, d, eps,
@@ -557,19 +560,18 @@ def rms_norm_grad(x, gain, dy, eps: float, need_dx: bool = True):
     return dx, dgain
 
 
-def _head(h, lm_head, targets):
-    import torch
-    dev, n, d, vocab = h.device, h.shape[0], h.shape[-1], lm_head.shape[0]
-    hs = _rows(h, "h", dev)
-    if _rows(lm_head, "lm_head", dev, d) != d or lm_head.dtype != h.dtype:
+def _head(h, lm_head, targets, int32):
+    dev, (n, d, hs) = h.device, _rows(h, "h")
+    vocab, _, ws = _rows(lm_head, "lm_head", dev, (None, d))
+    if ws != d or lm_head.dtype != h.dtype:
         raise ValueError(f"lm_head: contiguous rows of {h.dtype} are wanted, got {lm_head.dtype}, strides {lm_head.stride()}")
-    return dev, n, d, vocab, hs, _dtype_of(h, "h"), _flat(targets, "targets", dev, n, torch.int32)
+    return dev, n, d, vocab, hs, _dtype_of(h, "h"), _flat(targets, "targets", dev, n, int32)
 
 
 def head_loss(h, lm_head, targets):
     """ls_head_loss: (loss, lse), float32 [n] each, of h [n, d] through lm_head [vocab, d]; targets int32 [n], negative: skipped."""
     import torch
-    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets)
+    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets, torch.int32)
     loss = torch.empty(n, dtype=torch.float32, device=dev)
     lse = torch.empty(n, dtype=torch.float32, device=dev)
     nbytes = lib().ls_head_loss_workspace(n, d, vocab, dt, 0)
@@ -583,18 +585,19 @@ def head_loss_grad(h, lm_head, targets, weight, d_lm_head=None):
     """ls_head_loss_grad: (loss [n], dh [n, d], d_lm_head [vocab, d]) of sum(weight * loss); weight float32 [n].  d_lm_head: a tensor to
     overwrite (a new one otherwise)."""
     import torch
-    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets)
+    dev, n, d, vocab, hs, dt, tp = _head(h, lm_head, targets, torch.int32)
     wp = _flat(weight, "weight", dev, n, torch.float32)
     loss = torch.empty(n, dtype=torch.float32, device=dev)
-    dh = torch.empty((n, d), dtype=h.dtype, device=dev)
-    dw = _result(d_lm_head, "d_lm_head", (vocab, d), lm_head.dtype, dev)
-    if _rows(dw, "d_lm_head", dev, d) != d:
-        raise ValueError("d_lm_head: contiguous rows are wanted")
+    dh = h.new_empty((n, d))
+    if d_lm_head is None:
+        d_lm_head = lm_head.new_empty((vocab, d))
+    elif _rows(d_lm_head, "d_lm_head", dev, (vocab, d))[2] != d or d_lm_head.dtype != lm_head.dtype:
+        raise ValueError(f"d_lm_head: contiguous rows of {lm_head.dtype} are wanted")
     nbytes = lib().ls_head_loss_workspace(n, d, vocab, dt, 1)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _call(dev, "ls_head_loss_grad", h.data_ptr(), hs, lm_head.data_ptr(), dt, tp, wp, n, d, vocab, loss.data_ptr(), None,
-          dh.data_ptr(), d, dw.data_ptr(), ws.data_ptr(), nbytes)
-    return loss, dh, dw
+          dh.data_ptr(), d, d_lm_head.data_ptr(), ws.data_ptr(), nbytes)
+    return loss, dh, d_lm_head
 
 
 class AdamW:

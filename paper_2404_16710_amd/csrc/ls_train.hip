@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "ls_lanes.h"
 #include "ls_tiles.h"
@@ -15,6 +16,7 @@
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t bf16_t;
 
 namespace {

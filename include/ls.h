@@ -329,7 +329,7 @@ typedef struct { /* of one tensor */
   float *master;                   /* DEVICE float[n] or NULL                                    */
   void *m, *v;                     /* DEVICE, float[n] or uint8[n]                               */
   float *m_scale, *v_scale;        /* DEVICE float[(n + 255) / 256] (8 bits), ignored otherwise   */
-  int64_t n;                       /* elements; 0: skipped                                       */
+  int64_t n;                       /* elements, at most 2^40; 0: skipped                         */
   int32_t param_dtype, grad_dtype; /* LS_F32 or LS_BF16                                          */
 } ls_adam_tensor;
 typedef struct {

@@ -62,6 +62,20 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// Two sums at once; `red`: 8 pairs of LDS in two halves that take turns (`turn` alternates from call to call), so that one barrier
+// is enough.
+template <int TPR>
+__device__ __forceinline__ float2 row_sum2(float2 v, float2* red, int turn) {
+  v.x = wave_sum(v.x);
+  v.y = wave_sum(v.y);
+  if constexpr (TPR == 64) return v;
+  red += 4 * (turn & 1);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  const float2 a = red[0], b = red[1], c = red[2], d = red[3];
+  return make_float2((a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y));
+}
+
 #include "ls_head_mm.inc"
 #include "ls_norm.inc"
 #include "ls_head_loss.inc"
@@ -85,7 +99,7 @@ int ls_launch_norm_grad(const LsNormArgs& a, hipStream_t s) {
                   : (a.bf16 ? norm_grad_launch<float, bf16_t>(a, s) : norm_grad_launch<float, float>(a, s));
 }
 int ls_launch_norm_gain(const float* partial, int parts, int32_t d, int32_t bf16, void* dgain, hipStream_t s) {
-  const dim3 grid((d / 4 + 15) / 16);
+  const dim3 grid((d / 4 + 7) / 8);
   if (bf16) norm_gain_kernel<bf16_t><<<grid, dim3(256), 0, s>>>(partial, parts, d, static_cast<bf16_t*>(dgain));
   else norm_gain_kernel<float><<<grid, dim3(256), 0, s>>>(partial, parts, d, static_cast<float*>(dgain));
   return hipGetLastError() == hipSuccess ? 0 : 1;

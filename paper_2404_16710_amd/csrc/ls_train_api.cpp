@@ -105,7 +105,7 @@ int ls_adamw(const ls_adam_tensor* t, int32_t n_tensors, const ls_adam_config* c
       !std::isfinite(c->eps) || !std::isfinite(c->weight_decay) || !std::isfinite(c->grad_scale))
     return LS_E_RANGE;
   for (int32_t i = 0; i < n_tensors; ++i) {
-    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 42)) return LS_E_RANGE;
+    if (t[i].n < 0 || t[i].n > ((int64_t)1 << 40)) return LS_E_RANGE;
     if (t[i].n == 0) continue;
     if (!dtype_ok(t[i].param_dtype) || !dtype_ok(t[i].grad_dtype)) return LS_E_ARG;
     if (off16(t[i].param) || off16(t[i].grad) || off16(t[i].m) || off16(t[i].v) || (uintptr_t)t[i].master % 16) return LS_E_ARG;

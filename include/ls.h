@@ -333,7 +333,7 @@ typedef struct { /* of one tensor */
   int32_t param_dtype, grad_dtype; /* LS_F32 or LS_BF16                                          */
 } ls_adam_tensor;
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps > 0, lr and weight_decay finite and >= 0 */
+  double lr, beta1, beta2, eps, weight_decay, grad_scale; /* betas in [0, 1), eps >= 2^-126, lr and weight_decay >= 0 */
   int32_t step;                                           /* of this call, from 1               */
   int32_t state_bits;                                     /* 32 or 8                            */
 } ls_adam_config;

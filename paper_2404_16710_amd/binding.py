@@ -613,6 +613,8 @@ class AdamW:
             raise ValueError(f"bits: 8 or 32, got {bits}")
         if not len(params) == len(grads) == len(masters if masters is not None else params) == len(states if states is not None else params):
             raise ValueError("params, grads, masters and states: one of each for every tensor")
+        if len({p.data_ptr() for p in params if p.numel()}) != sum(1 for p in params if p.numel()):
+            raise ValueError("params: the same tensor twice")
         self.params, self.grads, self.masters, self.bits = list(params), list(grads), None if masters is None else list(masters), bits
         self.steps, self.lr, self.betas, self.eps, self.weight_decay = int(step), lr, betas, eps, weight_decay
         self.states = []

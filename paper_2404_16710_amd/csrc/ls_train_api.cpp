@@ -101,7 +101,7 @@ int ls_adamw(const ls_adam_tensor* t, int32_t n_tensors, const ls_adam_config* c
   if (n_tensors < 0 || c->step < 1) return LS_E_RANGE;
   if (c->state_bits != 32 && c->state_bits != 8) return LS_E_ARG;
   auto share = [](double b) { return b >= 0.0 && b < 1.0; };
-  if (!share(c->beta1) || !share(c->beta2) || !(c->eps > 0.0) || !(c->lr >= 0.0) || !(c->weight_decay >= 0.0) || !std::isfinite(c->lr) ||
+  if (!share(c->beta1) || !share(c->beta2) || !(c->eps >= 0x1p-126) || !(c->lr >= 0.0) || !(c->weight_decay >= 0.0) || !std::isfinite(c->lr) ||
       !std::isfinite(c->eps) || !std::isfinite(c->weight_decay) || !std::isfinite(c->grad_scale))
     return LS_E_RANGE;
   for (int32_t i = 0; i < n_tensors; ++i) {

@@ -157,7 +157,7 @@ def check_head(h, w, t, weight, dtype):
 
 
 HEAD_SHAPES = [(1, 16, 1), (1, 16, 17), (2, 48, 31), (1, 256, 1024), (16, 80, 100), (17, 64, 64), (45, 256, 1024), (5, 2048, 333), (64, 208, 1000),
-               (65, 128, 2064), (77, 1040, 4099), (130, 384, 257), (300, 96, 511), (333, 512, 1234), (513, 272, 8200), (1100, 64, 96)]
+               (65, 128, 2064), (77, 1040, 4099), (97, 144, 777), (128, 272, 130), (130, 384, 257), (300, 96, 511), (333, 512, 1234), (513, 272, 8200), (1100, 64, 96)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -479,3 +479,83 @@ def test_fp32_products_keep_24_bits():
     check(p, p[:, :1].expand_as(p), 18 * U * p.abs(), "dW / h")
     want = p[:1, :1] * w[0].double() + p[1:, :1] * w[1].double()
     check(dh[57], want[0], 18 * U * (p[:1, :1] * w[0].double()).abs()[0] + 18 * U * (p[1:, :1] * w[1].double()).abs()[0], "dh")
+
+
+def c_call(name, *args):
+    from paper_2404_16710_amd import binding as B
+    code = getattr(B.lib(), name)(*args, torch.cuda.current_stream().cuda_stream)
+    assert code == 0, (name, code)
+
+
+class Guarded:
+    """A buffer between two strips of a pattern, for writes that miss it."""
+
+    def __init__(self, nbytes, fill=0xA5):
+        self.all = torch.full((nbytes + 8192,), 0x5A, dtype=torch.uint8, device="cuda")
+        self.all[4096:4096 + nbytes] = fill
+        self.nbytes = nbytes
+
+    @property
+    def ptr(self):
+        return self.all.data_ptr() + 4096
+
+    def view(self, dtype, *shape):
+        return self.all[4096:4096 + self.nbytes].view(dtype).view(*shape)
+
+    def check(self):
+        assert (self.all[:4096] == 0x5A).all() and (self.all[4096 + self.nbytes:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, d, vocab", [(1, 16, 1), (3, 80, 77), (20, 208, 515), (70, 144, 1001), (130, 1040, 300), (300, 528, 65)])
+def test_nothing_is_written_outside_outputs_and_workspace(n, d, vocab, dtype):
+    """Through the C interface, with a workspace of exactly the size asked for that holds NaN, outputs in wider rows, and rows behind
+    the last one left as they were."""
+    from paper_2404_16710_amd import binding as B
+    T, code = TYPES[dtype], B.LS_BF16 if dtype == "bf16" else B.LS_F32
+    size = 2 if dtype == "bf16" else 4
+    h, w, t, weight = head_case(n, d, vocab, dtype, n + vocab)
+    loss, dh, dw, lse = Guarded(4 * n), Guarded(size * n * (d + 16)), Guarded(size * vocab * d), Guarded(4 * n)
+    nbytes = B.lib().ls_head_loss_workspace(n, d, vocab, code, 1)
+    ws = Guarded(nbytes, 0xFF)
+    c_call("ls_head_loss_grad", h.data_ptr(), d, w.data_ptr(), code, t.data_ptr(), weight.data_ptr(), n, d, vocab, loss.ptr, lse.ptr, dh.ptr,
+           d + 16, dw.ptr, ws.ptr, nbytes)
+    torch.cuda.synchronize()
+    for g in (loss, dh, dw, lse, ws):
+        g.check()
+    assert (dh.view(T, n, d + 16)[:, d:].view(torch.uint8) == 0xA5).all()
+    hd, wd, want, want_lse, dl, dlse, p, q, wt = head_reference(h, w, t, weight)
+    check(lse.view(torch.float32, n), want_lse, dlse, "lse")
+    assert not dh.view(T, n, d + 16)[:, :d].isnan().any() and not dw.view(T, vocab, d).isnan().any()
+    nbytes = B.lib().ls_head_loss_workspace(n, d, vocab, code, 0)
+    ws, again = Guarded(nbytes, 0xFF), Guarded(4 * n)
+    c_call("ls_head_loss", h.data_ptr(), d, w.data_ptr(), code, t.data_ptr(), n, d, vocab, again.ptr, None, ws.ptr, nbytes)
+    x, gain, y, dx, dgain = h.float(), w[0].contiguous(), Guarded(size * n * (d + 16)), Guarded(4 * n * (d + 16)), Guarded(size * d)
+    c_call("ls_rms_norm", x.data_ptr(), B.LS_F32, d, gain.data_ptr(), code, n, d, 1e-5, y.ptr, d + 16)
+    nbytes = B.lib().ls_rms_norm_grad_workspace(n, d)
+    ws2 = Guarded(nbytes, 0xFF)
+    c_call("ls_rms_norm_grad", x.data_ptr(), B.LS_F32, d, gain.data_ptr(), code, h.data_ptr(), d, n, d, 1e-5, dx.ptr, d + 16, dgain.ptr, ws2.ptr, nbytes)
+    torch.cuda.synchronize()
+    for g in (ws, again, y, dx, dgain, ws2):
+        g.check()
+    check(again.view(torch.float32, n), want, torch.where(t.long() >= 0, dl + dlse + 2 * U * want.abs(), 0.0), "loss")
+    assert (y.view(T, n, d + 16)[:, d:].view(torch.uint8) == 0xA5).all() and (dx.view(torch.float32, n, d + 16)[:, d:].view(torch.uint8) == 0xA5).all()
+
+
+def test_calls_on_two_streams_at_once():
+    from paper_2404_16710_amd import head_loss_grad, rms_norm_grad
+    cases = [head_case(n, 512, 3001, "bf16", n) for n in (40, 300)]
+    x = [normal(gen(i), 700, 1040) for i in range(2)]
+    gain = torch.ones(1040, device="cuda")
+    want = [[*head_loss_grad(*c), *rms_norm_grad(y, gain, y, 1e-5)] for c, y in zip(cases, x)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append([*head_loss_grad(*cases[i]), *rms_norm_grad(x[i], gain, x[i], 1e-5)])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for run in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(run, want[i]))

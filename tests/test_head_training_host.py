@@ -54,6 +54,8 @@ def test_workspaces_are_sized_for_supported_arguments_only():
     assert L.ls_rms_norm_grad_workspace(3, 64) >= 3 * 64 * 4 and L.ls_rms_norm_grad_workspace(0, 64) == 0 and L.ls_rms_norm_grad_workspace(3, 65) == 0
     size = L.ls_head_loss_workspace
     assert size(0, 64, 100, BF16, 0) == size(1, 64, 100, 3, 0) == size(1, 64, 100, BF16, 2) == size(1, 60, 100, BF16, 0) == size(1, 64, 0, BF16, 0) == 0
+    # many rows of a large vocabulary: at most 64 MB of statistics, or 256 rows
+    assert size(1 << 22, 64, 128256, BF16, 0) < 70 << 20 and size(1 << 22, 64, 1 << 21, BF16, 0) < 256 * (1 << 18) + (1 << 20)
     # no logits without gradients; with them at most about 4 GB of logits and p, however many rows
     assert 0 < size(4096, 4096, 32000, BF16, 0) < 16 << 20
     assert 4096 * 32000 * 6 <= size(4096, 4096, 32000, BF16, 1) < 4096 * 32000 * 6 + (64 << 20)
@@ -72,7 +74,7 @@ def adam(config=None, n_tensors=1, **tensor):
 
 
 @pytest.mark.parametrize("config, tensor, code", [
-    ({"step": 0}, {}, RANGE), ({"state_bits": 16}, {}, ARG), ({"beta1": 1.0}, {}, RANGE), ({"beta2": -0.1}, {}, RANGE), ({"eps": 0.0}, {}, RANGE),
+    ({"step": 0}, {}, RANGE), ({"state_bits": 16}, {}, ARG), ({"beta1": 1.0}, {}, RANGE), ({"beta2": -0.1}, {}, RANGE), ({"eps": 0.0}, {}, RANGE), ({"eps": 1e-40}, {}, RANGE),
     ({"lr": -1.0}, {}, RANGE), ({"lr": float("inf")}, {}, RANGE), ({"weight_decay": float("nan")}, {}, RANGE), ({"grad_scale": float("inf")}, {}, RANGE),
     ({}, {"n": -1}, RANGE), ({}, {"n": (1 << 42) + 1}, RANGE), ({}, {"param": None}, ARG), ({}, {"grad": 0x20008}, ARG), ({}, {"m": None}, ARG), ({}, {"v": 0x40004}, ARG),
     ({}, {"master": 0x80004}, ARG), ({}, {"param_dtype": 2}, ARG), ({}, {"grad_dtype": -1}, ARG),
@@ -110,5 +112,7 @@ def test_the_binding_refuses_tensors_that_are_not_what_it_needs():
         P.AdamW([x], [x])
     with pytest.raises(ValueError, match="one of each"):
         P.AdamW([x], [])
+    with pytest.raises(ValueError, match="twice"):
+        P.AdamW([x, x], [x, x])
     with pytest.raises(ValueError, match="8 or 32"):
         P.AdamW([x], [x], bits=16)

@@ -144,8 +144,9 @@ def check_head(h, w, t, weight, dtype):
     T = TYPES[dtype]
     n, vocab = p.shape
     # p: the exponential with the errors above, the subtraction, and in 16 bits its rounding (fp32: three planes, 2^-24)
-    dp = q * (dl + dlse + 290 * U)[:, None] + 2 * U * (q + p.abs()) + half(T) * p.abs()
-    planes = 6 if dtype == "f32" else 1
+    # (16 bits and at most 64 rows: two parts, 2^-17)
+    dp = q * (dl + dlse + 290 * U)[:, None] + 2 * U * (q + p.abs()) + (half(T) if dtype == "f32" or len(p) > 64 else 2.0 ** -17) * p.abs()
+    planes = 6 if dtype == "f32" else 2
     want = p @ wd
     tol = dp @ wd.abs() + (planes * vocab + 20) * U * (p.abs() @ wd.abs()) + half(T) * want.abs()
     check(dh, want, tol + 1e-30, "dh")
@@ -379,8 +380,9 @@ def test_exit_loss_of_a_text_and_a_step_of_the_head(dtype, n, ffn):
     again = gm.fit_exits(prompt, scales, opt, targets)
     assert (again == losses).all() or abs(again - losses).max() <= 2 * float(tol.max())
     T = TYPES[dtype]
-    dp = q * (dl + dlse + 290 * U)[:, None] + 2 * U * (q + p.abs()) + half(T) * p.abs()
-    planes = 6 if dtype == "f32" else 1
+    # (16 bits and at most 64 rows: two parts, 2^-17)
+    dp = q * (dl + dlse + 290 * U)[:, None] + 2 * U * (q + p.abs()) + (half(T) if dtype == "f32" or len(p) > 64 else 2.0 ** -17) * p.abs()
+    planes = 6 if dtype == "f32" else 2
     want = p.T @ hd
     d_head = opt.grads[0]
     check(d_head, want, dp.T @ hd.abs() + (planes * 2 * n + 20) * U * (p.T.abs() @ hd.abs()) + half(T) * want.abs() + 1e-30, "dW")

@@ -277,7 +277,8 @@ int ls_rms_norm(const void *dev_x, int32_t x_dtype, int64_t x_stride, const void
                 int32_t d, float eps, void *dev_y, int64_t y_stride, void *stream);
 
 /* Gradients of ls_rms_norm for dy (`dtype`): dx (x_dtype; NULL: not wanted) = r (gain dy) - x r^3 mean(gain dy x) and dgain
- * (`dtype`, [d]; NULL: not wanted, no workspace then) = sum over rows of dy x r.  Sums are fp32 in a fixed order. */
+ * (`dtype`, [d]; NULL: not wanted, no workspace then) = sum over rows of dy x r.  Sums are fp32 in a fixed order.
+ * A row whose dy is zero throughout has dx = 0 and adds nothing, whatever its x holds. */
 size_t ls_rms_norm_grad_workspace(int32_t n, int32_t d);
 int ls_rms_norm_grad(const void *dev_x, int32_t x_dtype, int64_t x_stride, const void *dev_gain, int32_t dtype,
                      const void *dev_dy, int64_t dy_stride, int32_t n, int32_t d, float eps, void *dev_dx, int64_t dx_stride,
@@ -292,7 +293,7 @@ int ls_head_loss(const void *dev_h, int64_t h_stride, const void *dev_lm_head, i
                  size_t workspace_bytes, void *stream);
 /* The same loss with the gradients of sum_i weight[i] * loss[i] (DEVICE float[n]; rows of several exits are stacked, with each
  * exit's scale in its rows' weights): p = weight * (softmax - [target]), dh = p W, dW = p^T h, both in `dtype`, both overwritten; a
- * skipped row adds nothing and its dh is 0; a target of vocab or more makes its dh and all of dW NaN.  For LS_BF16 p
+ * skipped row adds nothing, whatever stands in it, and its dh is 0; a target of vocab or more makes its dh and all of dW NaN.  For LS_BF16 p
  * enters the two products rounded to 16 bits (up to 64 rows: to 2^-17); their sums are fp32 and are rounded once. */
 int ls_head_loss_grad(const void *dev_h, int64_t h_stride, const void *dev_lm_head, int32_t dtype, const int32_t *dev_targets,
                       const float *dev_weight, int32_t n, int32_t d, int32_t vocab, float *dev_loss, float *dev_lse,

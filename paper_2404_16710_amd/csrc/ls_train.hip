@@ -62,18 +62,20 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Two sums at once; `red`: 8 pairs of LDS in two halves that take turns (`turn` alternates from call to call), so that one barrier
-// is enough.
+// Two sums at once, and whether any thread's `any` is set; `red`: two halves of LDS that take turns (`turn` alternates from call to
+// call), so that one barrier is enough.
+struct RowSums { float2 s; int any; };
 template <int TPR>
-__device__ __forceinline__ float2 row_sum2(float2 v, float2* red, int turn) {
+__device__ __forceinline__ RowSums row_sum2(float2 v, bool any, RowSums* red, int turn) {
   v.x = wave_sum(v.x);
   v.y = wave_sum(v.y);
-  if constexpr (TPR == 64) return v;
+  const int some = __any(any);
+  if constexpr (TPR == 64) return RowSums{v, some};
   red += 4 * (turn & 1);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = RowSums{v, some};
   __syncthreads();
-  const float2 a = red[0], b = red[1], c = red[2], d = red[3];
-  return make_float2((a.x + b.x) + (c.x + d.x), (a.y + b.y) + (c.y + d.y));
+  const RowSums a = red[0], b = red[1], c = red[2], d = red[3];
+  return RowSums{make_float2((a.s.x + b.s.x) + (c.s.x + d.s.x), (a.s.y + b.s.y) + (c.s.y + d.s.y)), a.any | b.any | c.any | d.any};
 }
 
 #include "ls_head_mm.inc"

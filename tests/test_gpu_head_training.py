@@ -95,6 +95,22 @@ def test_rms_norm_passes_on_what_is_not_finite_in_its_row_alone():
     assert torch.equal(got[[0, 2, 4]], want[[0, 2, 4]])
 
 
+@pytest.mark.parametrize("d", [64, 1040, 5120, 16400])
+def test_rows_whose_dy_is_zero_throughout_add_nothing_whatever_they_hold(d):
+    """Padding: skipped rows of a loss come back as zeros, and their states may be anything."""
+    from paper_2404_16710_amd import rms_norm_grad
+    g = gen(d)
+    n = 9
+    x, gain, dy = normal(g, n, d), normal(g, d, std=0.2, mean=1.0), normal(g, n, d)
+    dy[[0, 4, 8]] = 0
+    dy[4, 5] = -0.0
+    dx, dgain = rms_norm_grad(x, gain, dy, 1e-5)
+    bad = x.clone()
+    bad[0, 3], bad[4], bad[8, d - 1] = float("nan"), float("inf"), float("-inf")
+    got_dx, got_dgain = rms_norm_grad(bad, gain, dy, 1e-5)
+    assert torch.equal(got_dgain, dgain) and torch.equal(got_dx, dx) and (dx[[0, 4, 8]] == 0).all()
+
+
 # ---- Softmax cross entropy through the head ----------------------------------------------------------------------
 def head_case(n, d, vocab, dtype, seed, pad=0):
     g = gen(seed)
@@ -192,6 +208,22 @@ def test_head_rows_are_independent_of_what_else_is_not_finite(dtype):
         got = head_loss(h2, w, t)
         keep = torch.arange(n, device="cuda") != 5
         assert got[1][5].isnan() and torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[1][keep], want[1][keep])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n, d, vocab", [(4, 64, 100), (40, 208, 700), (70, 144, 300), (100, 1040, 515), (150, 128, 700), (333, 272, 1030)])
+def test_skipped_rows_may_hold_anything(n, d, vocab, dtype):
+    """Padding: what stands in a row without a target reaches neither the other rows nor dW."""
+    from paper_2404_16710_amd import head_loss_grad
+    h, w, t, weight = head_case(n, d, vocab, dtype, n, pad=16)
+    t[n - 1] = -1
+    want = head_loss_grad(h, w, t, weight)
+    for bad in (float("nan"), float("inf")):
+        h2, weight2 = h.clone(), weight.clone()
+        h2[1, 2], h2[n - 1], weight2[n - 1] = bad, bad, bad
+        got = head_loss_grad(h2, w, t, weight2)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("n, shift", [(3, 1000.0), (100, 1000.0), (100, -1000.0)])

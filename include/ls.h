@@ -272,7 +272,7 @@ size_t ls_static_workspace_limit(void);
  * outside its range; LS_E_CAPACITY: workspace too small.  Results depend on the arguments' values alone, not on the call. */
 
 /* y = x * r * gain with r = 1 / sqrt(mean(x^2) + eps), rounded once.  x has x_dtype (a context's captured states are LS_F32), gain
- * and y have `dtype`.  1 <= n <= 2^24 rows. */
+ * and y have `dtype`.  1 <= n <= 2^23 rows. */
 int ls_rms_norm(const void *dev_x, int32_t x_dtype, int64_t x_stride, const void *dev_gain, int32_t dtype, int32_t n,
                 int32_t d, float eps, void *dev_y, int64_t y_stride, void *stream);
 

@@ -6,7 +6,7 @@
 
 namespace {
 
-constexpr int32_t kMaxRows = 1 << 22, kMaxNormRows = 1 << 24, kMaxWidth = 65536, kMaxVocab = 1 << 21;
+constexpr int32_t kMaxRows = 1 << 22, kMaxNormRows = 1 << 23, kMaxWidth = 65536, kMaxVocab = 1 << 21;
 
 bool dtype_ok(int32_t t) { return t == LS_F32 || t == LS_BF16; }
 int64_t elem(int32_t t) { return t == LS_BF16 ? 2 : 4; }

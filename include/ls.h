@@ -15,6 +15,9 @@
  *     the drafted positions so that verification starts at layer E.
  *   - Appendix A.4: after a round the cache keeps (prompt + emitted - 1) positions.
  *
+ * A last section has the operators that the shared head g is trained with: norms, the softmax cross entropy of all exits' rows, their
+ * gradients, AdamW.
+ *
  * Conventions
  *   - Pointers marked DEVICE point to GPU memory the CALLER owns (weights, workspace, token
  *     buffers).  The library never allocates or frees device memory.  Pointers marked HOST are

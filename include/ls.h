@@ -290,7 +290,7 @@ int ls_rms_norm_grad(const void *dev_x, int32_t x_dtype, int64_t x_stride, const
 /* Softmax cross entropy of n rows through an LM head [vocab][d] (any vocab from 1 to 2^21), without keeping the logits:
  * lse[i] = log sum_v exp(h_i . W_v), loss[i] = lse[i] - h_i . W_target[i], both float[n] (dev_lse may be NULL).  dev_targets: DEVICE
  * int32[n]; a negative target skips the row (loss 0), one of vocab or more makes its loss NaN.  1 <= n <= 2^22.
- * Products and sums are fp32 (fp32 operands: 2^-24 of a product may be left out). */
+ * Products and sums are fp32 (fp32 operands: 2^-24 of a product may be left out, an infinite one gives NaN). */
 int ls_head_loss(const void *dev_h, int64_t h_stride, const void *dev_lm_head, int32_t dtype, const int32_t *dev_targets,
                  int32_t n, int32_t d, int32_t vocab, float *dev_loss, float *dev_lse, void *dev_workspace,
                  size_t workspace_bytes, void *stream);
